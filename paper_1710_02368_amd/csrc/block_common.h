@@ -22,6 +22,9 @@ inline int mask_threshold(float rate) {
   return t <= 65535 ? (int)t : -1;
 }
 
+// chunks of eight columns a row (any cols >= 0)
+inline uint32_t chunks_of(int32_t cols) { return ((uint32_t)cols + 7) / 8; }
+
 inline bool block_dtype_ok(int32_t d) { return d == AGN_FP32 || d == AGN_BF16; }
 inline bool element_aligned(const void* p, int32_t dtype) { return ((uintptr_t)p & (dtype == AGN_BF16 ? 1 : 3)) == 0; }
 
@@ -199,12 +202,12 @@ __device__ __forceinline__ void move_down(Raw8<float>& r, int d) {
     }
   if (d >= 4) r.a = blk_u32x4{0u, 0u, 0u, 0u};
 }
-// columns c .. c+7 of a row of `cols`, zeros past its end (c < cols)
+// columns c .. c+7 of a row of `cols`, zeros past its end (c < cols; c + 8 may pass 2^31)
 template <class T>
 __device__ __forceinline__ Raw8<T> load8_row(const T* row, int c, int cols) {
   if (cols < 8) return load8_part(row + c, cols - c);
   Raw8<T> r = load8(row + min(c, cols - 8));
-  if (c + 8 > cols) move_down(r, c + 8 - cols);
+  if (c > cols - 8) move_down(r, c - (cols - 8));
   return r;
 }
 
@@ -254,7 +257,7 @@ __device__ __forceinline__ void store8_part(float* p, const Raw8<float>& r, int 
 }
 template <class T>
 __device__ __forceinline__ void store8_row(T* row, int c, int cols, const Raw8<T>& r) {
-  if (c + 8 <= cols)
+  if (cols - c >= 8)
     store8(row + c, r);
   else
     store8_part(row + c, r, cols - c);

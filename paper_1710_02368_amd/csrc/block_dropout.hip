@@ -45,7 +45,7 @@ __global__ __launch_bounds__(256) void dropout_kernel(const T* x, int64_t ldx, T
 template <class T>
 void launch(const agn_dropout_args& a, hipStream_t s) {
   const MaskArgs m = mask_args(a.mask);
-  const uint32_t n8 = (uint32_t)((a.cols + 7) / 8);
+  const uint32_t n8 = chunks_of(a.cols);
   const int64_t slab = std::max<int64_t>(1, ((INT64_C(1) << 31) - 1) / n8);  // rows a launch
   for (int64_t r = 0; r < a.rows; r += slab) {
     const uint32_t items = (uint32_t)(std::min(slab, a.rows - r) * n8);

@@ -26,11 +26,12 @@ struct Tokens {
 constexpr int kZeroBlocks = 64;  // workgroups that clear the rows past the last place
 
 // rows of `y` from *total on become zero; workgroup b of kZeroBlocks
+// (columns are counted without a sign: the last step of a row of almost 2^31 passes 2^31)
 template <class T>
 __device__ __forceinline__ void clear_tail(T* y, int64_t ldy, const Tokens& a, int b) {
   const uint32_t total = (uint32_t)max(0, *a.total);
   for (uint32_t r = total + b; r < a.pairs; r += kZeroBlocks)
-    for (int c = threadIdx.x * 8; c < a.cols; c += 256 * 8) store8_row(y + (int64_t)r * ldy, c, a.cols, zero8(y));
+    for (uint32_t c = threadIdx.x * 8; c < (uint32_t)a.cols; c += 256 * 8) store8_row(y + (int64_t)r * ldy, c, a.cols, zero8(y));
 }
 
 // A thread takes eight columns of one row: one load, k stores.
@@ -107,7 +108,7 @@ __global__ __launch_bounds__(256) void combine_backward_kernel(Tokens a, int64_t
       w[j] = there ? a.weights[row * a.k + j0 + j] : 0.f;
       dot[j] = 0.f;
     }
-    for (int c = lane * 8; c < a.cols; c += 512) {
+    for (uint32_t c = lane * 8; c < (uint32_t)a.cols; c += 512) {
       const Raw8<T> gr = load8_row(x + row * a.ldx, c, a.cols);
       Raw8<T> yr[KB];
 #pragma unroll
@@ -165,7 +166,7 @@ void slabs(int64_t rows, uint32_t n8, F&& f) {
 
 template <class T>
 void launch_dispatch(const agn_tokens_args& a, hipStream_t s) {
-  const uint32_t n8 = (uint32_t)((a.cols + 7) / 8);
+  const uint32_t n8 = chunks_of(a.cols);
   slabs(a.rows, n8, [&](uint32_t r0, uint32_t items, bool last) {
     const uint32_t nblk = (items + 255) / 256;
     hipLaunchKernelGGL(dispatch_kernel<T>, dim3(nblk + (last ? kZeroBlocks : 0)), dim3(256), 0, s, tokens(a), r0, items,
@@ -174,7 +175,7 @@ void launch_dispatch(const agn_tokens_args& a, hipStream_t s) {
 }
 template <class T>
 void launch_combine(const agn_tokens_args& a, hipStream_t s) {
-  const uint32_t n8 = (uint32_t)((a.cols + 7) / 8);
+  const uint32_t n8 = chunks_of(a.cols);
   slabs(a.rows, n8, [&](uint32_t r0, uint32_t items, bool) {
     hipLaunchKernelGGL(combine_kernel<T>, dim3((items + 255) / 256), dim3(256), 0, s, tokens(a), r0, items,
                        fast_div(n8));
