@@ -6,7 +6,7 @@ import torch
 
 from tests import block_oracle as O
 from tests.helpers import require_gpu
-from tests.test_gpu_block import SEED
+from tests.test_gpu_block import BOTH, DTYPES, SEED, _check_norms, _norms_case
 
 pytestmark = pytest.mark.gpu
 
@@ -67,3 +67,47 @@ def test_tokens_of_the_widest_rows(cols):
     assert torch.equal(y[0], x[0]) and not y[1].any()
     back = block.combine(y, r)
     assert torch.equal(back, x * 0.5)
+
+
+# ---------------------------------------------------------------------------
+# infinities under the mask
+# ---------------------------------------------------------------------------
+
+@pytest.mark.parametrize("what", ["gate", "w_post"])
+@pytest.mark.parametrize("value", [float("inf"), float("nan")])
+@BOTH
+@pytest.mark.parametrize("cols", [64, 517, 5000])
+def test_norms_factors_of_dropped_elements(cols, dtype, value, what):
+    """A dropped element is 0 whatever its factors are: an infinite or NaN gate
+    or weight there gives the bits of a finite one, in both directions.  (w_post
+    is a value a column: one row, so that no kept element has it.)"""
+    block = _block()
+    rows, rate = (6, 0.4) if what == "gate" else (1, 0.4)
+    keep = O.mask(rows, cols, rate, SEED, 3)
+    g = torch.Generator().manual_seed(cols)
+    rand = lambda *s: torch.randn(*s, generator=g)
+    r, f, dres, dh, gate = (rand(rows, cols).to(DTYPES[dtype]).cuda() for _ in range(5))
+    w_post, w_pre = (1 + 0.1 * rand(cols)).cuda(), (1 + 0.1 * rand(cols)).cuda()
+    dropped = (keep == 0).cuda()
+    assert dropped.any() and not dropped.all()
+
+    def both(gate, w_post):
+        kw = dict(gate=gate, alpha=0.5, dropout=(rate, SEED, 3))
+        res, h, saved = block.norms(r, f, w_post, w_pre, **kw)
+        return (res, h, *block.norms_backward(dres, dh, res, f, w_post, w_pre, saved, **kw))
+
+    want = both(gate, w_post)
+    if what == "gate":
+        got = both(torch.where(dropped, value, gate.float()).to(DTYPES[dtype]), w_post)
+    else:
+        got = both(gate, torch.where(dropped[0], value, w_post))
+    for i, (a, b) in enumerate(zip(got, want)):
+        assert torch.isfinite(b).all() and torch.equal(a, b), i
+
+
+@BOTH
+@pytest.mark.parametrize("rows,cols", [(1100, 4096), (1100, 4100), (700, 8192), (1300, 2056)])
+@pytest.mark.parametrize("gate", ["channel", "full"])
+def test_norms_many_wide_rows(rows, cols, gate, dtype):
+    """Teams of 8 and 16 waves that walk several rows each."""
+    _check_norms(_block(), *_norms_case(rows, cols, dtype, gate), 0.1, dtype)
