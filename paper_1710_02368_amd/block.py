@@ -173,6 +173,13 @@ def _workspace(name, device, *sizes):
 
 
 _DTYPES = {torch.float32: AGN_FP32, torch.bfloat16: AGN_BF16}
+_MOST = 0x7FFFFFFF  # the structs' 32-bit sizes (ctypes would drop what lies above)
+
+
+def _size(n, name):
+    if not 0 <= n <= _MOST:
+        raise ValueError(f"{name} must be in [0, 2^31), not {n}")
+    return n
 
 
 def _matrix(t, name, rows=None, cols=None, like=None):
@@ -181,6 +188,8 @@ def _matrix(t, name, rows=None, cols=None, like=None):
     if len(shape) != 2 or (rows is not None and shape[0] != rows) or (cols is not None and shape[1] != cols):
         want = "2-D" if rows is None or cols is None else f"{rows} x {cols}"
         raise ValueError(f"{name} must be {want}, not {tuple(shape)}")
+    if shape[1] > _MOST:
+        raise ValueError(f"{name} must have fewer than 2^31 columns, not {shape[1]}")
     if like is not None:
         if t.dtype is not like.dtype or t.get_device() != like.get_device():
             raise ValueError(f"{name} must be {like.dtype} on {like.device}, not {t.dtype} on {t.device}")
@@ -366,6 +375,7 @@ def route(logits, k: int, over_all: bool = False) -> Route:
     lp, lld = _matrix(logits, "logits")
     rows, experts = logits.shape
     dev = logits.device
+    _size(k, "k")
     ws, wsp, nws = _workspace("agn_route_workspace", dev, rows, experts, k)
     chosen = _new(rows, k, torch.int32, dev)
     weights = _new(rows, k, torch.float32, dev)
@@ -383,6 +393,7 @@ def route_chosen(chosen, weights, experts: int) -> Route:
         raise ValueError(f"chosen must be rows x k on a ROCm device, not {tuple(chosen.shape)} on {chosen.device}")
     rows, k = chosen.shape
     dev = chosen.device
+    _size(experts, "experts")
     cp = _vector(chosen, "chosen", (rows, k), dev, torch.int32)
     if weights is not None:
         _vector(weights, "weights", (rows, k), dev)
@@ -478,6 +489,8 @@ def _experts_weights(w, x):
     if w.dim() != 3 or w.dtype != x.dtype or w.device != x.device:
         raise ValueError(f"w must be experts x outputs x inputs, {x.dtype} on {x.device}")
     e, o, i = w.shape
+    if max(e, o, i) > _MOST:
+        raise ValueError(f"w: every size must be below 2^31, not {tuple(w.shape)}")
     se, ld, step = w.stride()
     if o == 1:
         ld = se if e > 1 else max(i, 1)

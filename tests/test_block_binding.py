@@ -1,0 +1,36 @@
+"""What the block operators' binding refuses before it reaches the library
+(no device is needed: the arguments are looked at first)."""
+import pytest
+import torch
+
+from paper_1710_02368_amd import block
+
+
+def _meta(*shape, dtype=torch.bfloat16):
+    return torch.empty(*shape, dtype=dtype, device="meta")
+
+
+@pytest.mark.parametrize("cols", [1 << 31, 1 << 32, (1 << 32) + 8])
+def test_widths_that_the_structs_cannot_hold(cols):
+    """A width of 2^32 + 8 would arrive as 8, and most of the output would stay unwritten."""
+    for call in (lambda: block.dropout(_meta(1, cols), 0.1, 1, 1),
+                 lambda: block.norms(_meta(1, cols), None, None, None),
+                 lambda: block.route(_meta(1, cols), 2),
+                 lambda: block.dispatch(_meta(1, cols), None),
+                 lambda: block.experts(_meta(1, cols), None, None)):
+        with pytest.raises(ValueError, match="fewer than 2\\^31 columns"):
+            call()
+    for shape in ((1, 1, cols), (1, cols, 1), (cols, 1, 1)):
+        with pytest.raises(ValueError, match="w: every size"):
+            block._experts_weights(_meta(*shape), _meta(1, 1))
+
+
+@pytest.mark.parametrize("n", [-1, 1 << 31, (1 << 32) + 2])
+def test_counts_that_the_structs_cannot_hold(n):
+    class Device(torch.Tensor):  # (stands for a tensor on the device)
+        is_cuda = True
+
+    with pytest.raises(ValueError, match="k must be in"):
+        block.route(_meta(4, 8).as_subclass(Device), n)
+    with pytest.raises(ValueError, match="experts must be in"):
+        block.route_chosen(_meta(4, 2, dtype=torch.int32).as_subclass(Device), None, n)
