@@ -428,8 +428,9 @@ def _tokens(name, r, rows, cols, x, y, like, weights, dy=None, dweights=None):
     k = r.slot.shape[1]
     dev = like.device
     sp = _vector(r.slot, "slot", (rows, k), dev, torch.int32)
-    if r.offsets.dtype != torch.int32 or r.offsets.device != dev or not r.offsets.is_contiguous():
-        raise ValueError(f"offsets must be contiguous int32 on {dev}")
+    if (r.offsets.dtype != torch.int32 or r.offsets.device != dev or r.offsets.dim() != 1 or r.offsets.numel() < 2
+            or not r.offsets.is_contiguous()):
+        raise ValueError(f"offsets must be a contiguous int32 vector of experts + 1 on {dev}")
     wp = None
     if weights:
         if r.weights is None:

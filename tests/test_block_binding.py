@@ -34,3 +34,14 @@ def test_counts_that_the_structs_cannot_hold(n):
         block.route(_meta(4, 8).as_subclass(Device), n)
     with pytest.raises(ValueError, match="experts must be in"):
         block.route_chosen(_meta(4, 2, dtype=torch.int32).as_subclass(Device), None, n)
+
+
+@pytest.mark.parametrize("offsets", [torch.empty(0, dtype=torch.int32), torch.zeros(1, dtype=torch.int32),
+                                     torch.zeros(2, 2, dtype=torch.int32)], ids=["empty", "one", "matrix"])
+def test_offsets_without_a_last_one(offsets):
+    """The count of places in use is read from the last of experts + 1 offsets."""
+    slot = torch.zeros(3, 2, dtype=torch.int32)
+    r = block.Route(slot, None, offsets, slot.reshape(-1), slot)
+    x = torch.zeros(3, 8)
+    with pytest.raises(ValueError, match="offsets"):
+        block._tokens("agn_dispatch", r, 3, 8, (x.data_ptr(), 8), (x.data_ptr(), 8), x, False)
