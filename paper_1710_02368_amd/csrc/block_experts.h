@@ -2,6 +2,7 @@
 #pragma once
 
 #include "block_common.h"
+#include "row_tiles.h"
 
 namespace agn {
 
@@ -44,65 +45,6 @@ hipError_t launch_product_f32(int prod, const ProductArgs& g, hipStream_t s);
 constexpr int kTailBlocks = 64;  // workgroups that clear the output rows of no expert
 
 namespace {
-
-__device__ __forceinline__ int clamped_offset(const ProductArgs& g, int e) { return min(max(g.offsets[e], 0), g.rows); }
-
-// The tiles of TR rows of all experts, counted expert by expert.  Every lane
-// holds up to 64 experts' part of the count (one load of the offsets where
-// there are no more; the functions are called with every lane active and
-// give every lane the same).
-struct RowTile {
-  int e, r0, rend;   // expert (-1: no such tile), first row, the expert's end
-  int of, of_expert;  // the tile's number among its expert's, and how many those are
-};
-struct RowTiles {
-  int TR;                // rows a tile
-  int first, end, upto;  // this lane's expert's rows; tiles up to and with it (of the 64 at e0)
-  int e0, base;          // the loaded experts' first; tiles before it
-  int total;             // tiles of all experts
-
-  __device__ void load(const ProductArgs& g, int at) {
-    const int lane = threadIdx.x & 63, e = at + lane;
-    first = end = 0;
-    if (e < g.experts) {
-      first = clamped_offset(g, e);
-      end = max(first, clamped_offset(g, e + 1));
-    }
-    upto = (end - first + TR - 1) / TR;
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-      const int o = __shfl_up(upto, d);
-      if (lane >= d) upto += o;
-    }
-    e0 = at;
-  }
-  __device__ void init(const ProductArgs& g, int rows_a_tile) {
-    TR = rows_a_tile;
-    total = 0;
-    for (int at = 0; at < g.experts; at += 64) {
-      base = total;
-      load(g, at);
-      total += __builtin_amdgcn_readlane(upto, 63);
-    }
-  }
-  __device__ RowTile find(const ProductArgs& g, int tile) {
-    if (g.experts > 64) {
-      base = 0;
-      for (int at = 0; at < g.experts; at += 64) {
-        load(g, at);
-        const int n = __builtin_amdgcn_readlane(upto, 63);
-        if (tile < base + n) break;
-        base += n;
-      }
-    }
-    const uint64_t hit = __ballot(tile < base + upto);
-    if (!hit) return {-1, 0, 0, 0, 0};
-    const int l = __builtin_ctzll(hit);
-    const int b = __builtin_amdgcn_readlane(first, l), en = __builtin_amdgcn_readlane(end, l);
-    const int n = (en - b + TR - 1) / TR, of = tile - base - __builtin_amdgcn_readlane(upto, l) + n;
-    return {e0 + l, b + of * TR, en, of, n};
-  }
-};
 
 // The rows, tile and output of workgroup `pid` of the weight gradients, whose
 // tiles are `per` an expert.

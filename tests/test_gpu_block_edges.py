@@ -6,7 +6,7 @@ import torch
 
 from tests import block_oracle as O
 from tests.helpers import require_gpu
-from tests.test_gpu_block import BOTH, DTYPES, SEED, _check_norms, _norms_case
+from tests.test_gpu_block import BOTH, DTYPES, SEED, _check_experts, _check_norms, _norms_case
 
 pytestmark = pytest.mark.gpu
 
@@ -111,3 +111,24 @@ def test_norms_factors_of_dropped_elements(cols, dtype, value, what):
 def test_norms_many_wide_rows(rows, cols, gate, dtype):
     """Teams of 8 and 16 waves that walk several rows each."""
     _check_norms(_block(), *_norms_case(rows, cols, dtype, gate), 0.1, dtype)
+
+
+# ---------------------------------------------------------------------------
+# the experts' products: more experts than a wave has lanes
+# ---------------------------------------------------------------------------
+
+def _mostly_the_last(experts, rows):
+    """Two rows to the first expert, one to the 64th, the rest to the last two."""
+    counts = [0] * experts
+    counts[0], counts[63], counts[-2] = 2, 1, (rows - 3) // 3
+    counts[-1] = rows - sum(counts)
+    return counts
+
+
+@BOTH
+@pytest.mark.parametrize("experts", [65, 130, 1024])
+@pytest.mark.parametrize("rows,i,o", [(64, 200, 72), (300, 72, 130), (800, 40, 72)])
+def test_many_experts(experts, rows, i, o, dtype):
+    """Few rows and many, nearly all of them in the last group of 64 experts."""
+    counts = _mostly_the_last(experts, rows - 5)
+    _check_experts(_block(), rows, counts, i, o, True, 0.1, "plain", dtype)
