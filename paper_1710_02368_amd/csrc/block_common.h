@@ -47,6 +47,11 @@ inline const char* rows_error(const agn_rows& m, int64_t rows, int64_t cols, int
     if (const char* e_ = ::agn::rows_error(m, rows, cols, dtype))                                          \
       return ::agn::block_fail(AGN_EINVAL, fn, e_, name);                                                  \
   } while (0)
+// a vector of 32-bit elements (null: nothing to look at)
+#define AGN_BLOCK_VECTOR(p, fn, name)                                                                   \
+  do {                                                                                                  \
+    if ((uintptr_t)(p) & 3) return ::agn::block_fail(AGN_EINVAL, fn, "pointer not aligned to its element", name); \
+  } while (0)
 
 // the mask as the kernels take it: threshold 0 draws nothing
 struct MaskArgs {

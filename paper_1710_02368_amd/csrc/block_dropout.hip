@@ -67,6 +67,7 @@ extern "C" int agn_dropout(const agn_dropout_args* a, void* stream) {
   AGN_BLOCK_REQUIRE(block_dtype_ok(a->dtype), fn, "dtype must be AGN_FP32 or AGN_BF16");
   AGN_BLOCK_REQUIRE(a->rows >= 0 && a->cols >= 0, fn, "negative size");
   AGN_BLOCK_REQUIRE(mask_threshold(a->mask.rate) >= 0, fn, "rate must be in [0, 1), below 1 - 2^-17");
+  AGN_BLOCK_VECTOR(a->mask.step_dev, fn, "step_dev");
   AGN_BLOCK_ROWS(a->x, a->rows, a->cols, a->dtype, fn, "x");
   AGN_BLOCK_ROWS(a->out, a->rows, a->cols, a->dtype, fn, "out");
   if (a->rows == 0 || a->cols == 0) return AGN_OK;

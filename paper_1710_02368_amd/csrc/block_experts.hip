@@ -196,6 +196,8 @@ extern "C" int agn_experts(const agn_experts_args* a, void* stream) {
   AGN_BLOCK_REQUIRE(a->relu == 0 || a->relu == 1, fn, "relu must be 0 or 1");
   AGN_BLOCK_REQUIRE(mask_threshold(a->mask.rate) >= 0, fn, "rate must be in [0, 1), below 1 - 2^-17");
   AGN_BLOCK_REQUIRE(element_aligned(a->bias, AGN_FP32), fn, "bias not aligned to its element");
+  AGN_BLOCK_VECTOR(a->mask.step_dev, fn, "step_dev");
+  AGN_BLOCK_VECTOR(a->offsets, fn, "offsets");
   AGN_BLOCK_ROWS(a->x, a->rows, a->inputs, a->dtype, fn, "x");
   AGN_BLOCK_ROWS(a->out, a->rows, a->outputs, a->dtype, fn, "out");
   if (a->rows == 0) return AGN_OK;
@@ -240,6 +242,7 @@ extern "C" int agn_experts_backward(const agn_experts_grad_args* a, void* stream
   AGN_BLOCK_REQUIRE(element_aligned(a->dw, AGN_FP32) && element_aligned(a->dbias, AGN_FP32), fn,
                     "dw or dbias not aligned to its element");
   AGN_BLOCK_REQUIRE(a->offsets, fn, "null offsets");
+  AGN_BLOCK_VECTOR(a->offsets, fn, "offsets");
   AGN_BLOCK_ROWS(a->dy, a->rows, a->outputs, a->dtype, fn, "dy");
   if (a->dw || a->relu_input) AGN_BLOCK_ROWS(a->x, a->rows, a->inputs, a->dtype, fn, "x");
   if (a->dx.p && a->rows > 0) {

@@ -427,6 +427,9 @@ int check(const agn_norms_args& a, bool grad, const char* fn) {
   AGN_BLOCK_REQUIRE(mask_threshold(a.mask.rate) >= 0, fn, "rate must be in [0, 1), below 1 - 2^-17");
   AGN_BLOCK_REQUIRE(element_aligned(a.w_post, AGN_FP32) && element_aligned(a.w_pre, AGN_FP32), fn,
                     "weights not aligned to their element");
+  AGN_BLOCK_VECTOR(a.mask.step_dev, fn, "step_dev");
+  AGN_BLOCK_VECTOR(a.rstd_post, fn, "rstd_post");
+  AGN_BLOCK_VECTOR(a.rstd_pre, fn, "rstd_pre");
   if (a.rows == 0) return AGN_OK;  // (pointers of nothing may be null: the parts cannot be told)
   if (a.f.p) {
     AGN_BLOCK_ROWS(a.f, a.rows, a.cols, a.dtype, fn, "f");
@@ -509,7 +512,12 @@ extern "C" int agn_norms_backward(const agn_norms_grad_args* a, void* stream) {
     AGN_BLOCK_REQUIRE(a->dw_post, fn, "null dw_post");
     AGN_BLOCK_REQUIRE(f.rstd_post || f.rows == 0, fn, "null rstd_post");
   }
-  if (f.gate_kind == AGN_GATE_CHANNEL) AGN_BLOCK_REQUIRE(a->dgate.p, fn, "null dgate");
+  AGN_BLOCK_VECTOR(a->dw_pre, fn, "dw_pre");
+  AGN_BLOCK_VECTOR(a->dw_post, fn, "dw_post");
+  if (f.gate_kind == AGN_GATE_CHANNEL) {
+    AGN_BLOCK_REQUIRE(a->dgate.p, fn, "null dgate");
+    AGN_BLOCK_VECTOR(a->dgate.p, fn, "dgate");
+  }
   if (has_f && f.gate_kind == AGN_GATE_FULL) AGN_BLOCK_ROWS(a->dgate, f.rows, f.cols, f.dtype, fn, "dgate");
   float* dgate = f.gate_kind == AGN_GATE_CHANNEL ? (float*)a->dgate.p : nullptr;
   float* dw_post = f.w_post ? a->dw_post : nullptr;

@@ -436,15 +436,20 @@ extern "C" int agn_route(const agn_route_args* a, void* stream) {
   if (const int e = check_sizes(a->rows, a->experts, a->k, fn)) return e;
   AGN_BLOCK_REQUIRE(a->over_all == 0 || a->over_all == 1, fn, "over_all must be 0 or 1");
   AGN_BLOCK_REQUIRE(a->offsets, fn, "null offsets");
+  AGN_BLOCK_VECTOR(a->offsets, fn, "offsets");
   const hipStream_t s = (hipStream_t)stream;
   if (a->rows == 0) {
     hipLaunchKernelGGL(no_pairs_kernel, dim3(1), dim3(256), 0, s, a->offsets, a->experts + 1);
     return block_launched(fn);
   }
   AGN_BLOCK_REQUIRE(a->chosen && a->source && a->slot, fn, "null chosen, source or slot");
+  AGN_BLOCK_VECTOR(a->chosen, fn, "chosen");
+  AGN_BLOCK_VECTOR(a->source, fn, "source");
+  AGN_BLOCK_VECTOR(a->slot, fn, "slot");
   if (a->logits.p) {
     AGN_BLOCK_REQUIRE(block_dtype_ok(a->dtype), fn, "dtype must be AGN_FP32 or AGN_BF16");
     AGN_BLOCK_REQUIRE(a->weights, fn, "null weights");
+    AGN_BLOCK_VECTOR(a->weights, fn, "weights");
     AGN_BLOCK_ROWS(a->logits, a->rows, a->experts, a->dtype, fn, "logits");
   }
   const int64_t need = agn_route_workspace(a->rows, a->experts, a->k);
@@ -490,6 +495,9 @@ extern "C" int agn_route_backward(const agn_route_grad_args* a, void* stream) {
   AGN_BLOCK_REQUIRE(a->over_all == 0 || a->over_all == 1, fn, "over_all must be 0 or 1");
   if (a->rows == 0) return AGN_OK;
   AGN_BLOCK_REQUIRE(a->chosen && a->weights && a->dweights, fn, "null chosen, weights or dweights");
+  AGN_BLOCK_VECTOR(a->chosen, fn, "chosen");
+  AGN_BLOCK_VECTOR(a->weights, fn, "weights");
+  AGN_BLOCK_VECTOR(a->dweights, fn, "dweights");
   if (a->over_all) AGN_BLOCK_ROWS(a->logits, a->rows, a->experts, a->dtype, fn, "logits");
   AGN_BLOCK_ROWS(a->dlogits, a->rows, a->experts, a->dtype, fn, "dlogits");
   if (a->dtype == AGN_BF16)

@@ -152,6 +152,8 @@ int check(const agn_tokens_args* a, const char* fn) {
   AGN_BLOCK_REQUIRE(a->rows < (INT64_C(1) << 31) / a->k, fn, "rows * k must be below 2^31");
   if (a->rows == 0) return AGN_OK;
   AGN_BLOCK_REQUIRE(a->slot && a->total, fn, "null plan");
+  AGN_BLOCK_VECTOR(a->slot, fn, "slot");
+  AGN_BLOCK_VECTOR(a->total, fn, "total");
   AGN_BLOCK_ROWS(a->x, a->rows, a->cols, a->dtype, fn, "x");
   AGN_BLOCK_ROWS(a->y, a->rows * a->k, a->cols, a->dtype, fn, "y");
   return AGN_OK;
@@ -216,6 +218,7 @@ extern "C" int agn_dispatch(const agn_tokens_args* a, void* stream) {
 extern "C" int agn_combine(const agn_tokens_args* a, void* stream) {
   const char* fn = "agn_combine";
   if (const int e = check(a, fn)) return e;
+  AGN_BLOCK_VECTOR(a->weights, fn, "weights");
   if (a->rows == 0 || a->cols == 0) return AGN_OK;
   if (a->dtype == AGN_BF16)
     launch_combine<uint16_t>(*a, (hipStream_t)stream);
@@ -229,6 +232,8 @@ extern "C" int agn_combine_backward(const agn_tokens_args* a, void* stream) {
   if (const int e = check(a, fn)) return e;
   if (a->rows == 0) return AGN_OK;
   AGN_BLOCK_REQUIRE(a->weights && a->dweights, fn, "null weights or dweights");
+  AGN_BLOCK_VECTOR(a->weights, fn, "weights");
+  AGN_BLOCK_VECTOR(a->dweights, fn, "dweights");
   AGN_BLOCK_ROWS(a->dy, a->rows * a->k, a->cols, a->dtype, fn, "dy");
   if (a->dtype == AGN_BF16)
     launch_combine_backward<uint16_t>(*a, (hipStream_t)stream);
