@@ -324,6 +324,8 @@ def norms_backward(dresidual_out, dh, residual_out, f, w_post, w_pre, saved, gat
     if w_pre is not None:
         wi = _vector(w_pre, "w_pre", (cols,), dev)
         rpr = rs + 4 * rows
+        if dh is None:
+            raise ValueError("dh must be given with w_pre")
         hp, hld = _matrix(dh, "dh", rows, cols, like=residual_out)
         dw_pre = _new_vector(cols, dev)
     rp = rld = None
@@ -411,6 +413,7 @@ def route_backward(logits, r: Route, dweights, over_all: bool = False):
     rows, experts = logits.shape
     dev = logits.device
     k = r.chosen.shape[1]
+    _has_weights(r)
     dl = _new(rows, experts, logits.dtype, dev)
     a = agn_route_grad_args(rows, experts, k, _DTYPES[logits.dtype], int(over_all), lp, lld,
                             _vector(r.chosen, "chosen", (rows, k), dev, torch.int32),
@@ -424,6 +427,11 @@ def route_backward(logits, r: Route, dweights, over_all: bool = False):
 # rows to their experts and back
 # --------------------------------------------------------------------------
 
+def _has_weights(r):
+    if r.weights is None:
+        raise ValueError("the route has no weights")
+
+
 def _tokens(name, r, rows, cols, x, y, like, weights, dy=None, dweights=None):
     k = r.slot.shape[1]
     dev = like.device
@@ -433,8 +441,7 @@ def _tokens(name, r, rows, cols, x, y, like, weights, dy=None, dweights=None):
         raise ValueError(f"offsets must be a contiguous int32 vector of experts + 1 on {dev}")
     wp = None
     if weights:
-        if r.weights is None:
-            raise ValueError("the route has no weights")
+        _has_weights(r)
         wp = _vector(r.weights, "weights", (rows, k), dev)
     a = agn_tokens_args(rows, cols, k, _DTYPES[like.dtype], sp, r.offsets.data_ptr() + 4 * (r.offsets.numel() - 1), wp,
                         *x, *y, *(dy or (None, 0)), dweights)

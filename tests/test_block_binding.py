@@ -25,11 +25,13 @@ def test_widths_that_the_structs_cannot_hold(cols):
             block._experts_weights(_meta(*shape), _meta(1, 1))
 
 
+class Device(torch.Tensor):
+    """Stands for a tensor on the device."""
+    is_cuda = True
+
+
 @pytest.mark.parametrize("n", [-1, 1 << 31, (1 << 32) + 2])
 def test_counts_that_the_structs_cannot_hold(n):
-    class Device(torch.Tensor):  # (stands for a tensor on the device)
-        is_cuda = True
-
     with pytest.raises(ValueError, match="k must be in"):
         block.route(_meta(4, 8).as_subclass(Device), n)
     with pytest.raises(ValueError, match="experts must be in"):
@@ -45,3 +47,16 @@ def test_offsets_without_a_last_one(offsets):
     x = torch.zeros(3, 8)
     with pytest.raises(ValueError, match="offsets"):
         block._tokens("agn_dispatch", r, 3, 8, (x.data_ptr(), 8), (x.data_ptr(), 8), x, False)
+
+
+def test_gradients_of_what_is_not_there():
+    """Choices without weights, norms before a block without the gradient of their output."""
+    chosen = _meta(3, 2, dtype=torch.int32)
+    logits = _meta(3, 8, dtype=torch.float32).as_subclass(Device)
+    r = block.Route(chosen, None, _meta(9, dtype=torch.int32), chosen.reshape(-1), chosen)
+    with pytest.raises(ValueError, match="no weights"):
+        block.route_backward(logits, r, _meta(3, 2, dtype=torch.float32))
+    x, w = _meta(3, 8, dtype=torch.float32).as_subclass(Device), _meta(8, dtype=torch.float32)
+    saved = block.NormsSaved(_meta(2, 3, dtype=torch.float32), x)
+    with pytest.raises(ValueError, match="dh must"):
+        block.norms_backward(None, None, x, None, None, w, saved)
