@@ -32,8 +32,8 @@ import torch
 
 from .agn import AGN_BF16, AGN_FP32, AGNError, load_library
 
-__all__ = ["Route", "dropout", "norms", "norms_backward", "route", "route_backward", "dispatch",
-           "dispatch_backward", "combine", "combine_backward", "experts", "experts_backward", "EXPORTED"]
+__all__ = ["NormsSaved", "Route", "dropout", "norms", "norms_backward", "route", "route_chosen", "route_backward",
+           "dispatch", "dispatch_backward", "combine", "combine_backward", "experts", "experts_backward", "EXPORTED"]
 
 EXPORTED = [
     "agn_block_error", "agn_dropout", "agn_norms", "agn_norms_backward_workspace", "agn_norms_backward",

@@ -60,3 +60,9 @@ def test_gradients_of_what_is_not_there():
     saved = block.NormsSaved(_meta(2, 3, dtype=torch.float32), x)
     with pytest.raises(ValueError, match="dh must"):
         block.norms_backward(None, None, x, None, None, w, saved)
+
+
+def test_every_public_name_is_listed():
+    own = {n for n, v in vars(block).items() if not n.startswith(("_", "agn_")) and callable(v)
+           and getattr(v, "__module__", "") == block.__name__}
+    assert own == set(block.__all__) - {"EXPORTED"}
