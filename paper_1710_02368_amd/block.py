@@ -5,6 +5,9 @@ device, makes the output tensors (uninitialised memory of torch's allocator on
 the current stream, which the kernels fill), and enqueues the work on the
 current stream of the tensors' device without waiting.
 
+The calls stand outside autograd, each gradient being a call of its own: what
+they return is not connected to inputs that require gradients.
+
 Matrices of rows are 2-D tensors of float32 or bfloat16 with adjacent columns
 (stride(1) == 1); rows may be strided.  Other strides are refused, not copied.
 ``dropout`` arguments are (rate, seed, step) or (rate, seed, step, step_dev),
@@ -225,18 +228,24 @@ def _mask(dropout, device):
 
 def dropout(x, rate: float, seed: int, step: int, out=None, step_dev=None):
     """mask * x; the gradient is dropout(dy) with the same rate, seed and step.
-    out: written instead of a new tensor (may be x)."""
+    out: written instead of a new tensor (may be x); like torch's own, it must
+    not require gradients while they are recorded, and counts as modified."""
     xp, xld = _matrix(x, "x")
     dev = x.device
     rows, cols = x.shape
     dtype = x.dtype
-    if out is None:
+    given = out is not None
+    if not given:
         out = _new(rows, cols, dtype, dev)
         op, old = out.data_ptr(), cols
     else:
         op, old = _matrix(out, "out", rows, cols, like=x)
+        if out.requires_grad and torch.is_grad_enabled():
+            raise ValueError("out requires gradients, and the call is not recorded")
     a = agn_dropout_args(rows, cols, _DTYPES[dtype], xp, xld, op, old, *_mask((rate, seed, step, step_dev), dev))
     _call("agn_dropout", a, dev.index)
+    if given:
+        torch.autograd.graph.increment_version(out)
     return out
 
 

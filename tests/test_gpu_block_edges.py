@@ -132,3 +132,29 @@ def test_many_experts(experts, rows, i, o, dtype):
     """Few rows and many, nearly all of them in the last group of 64 experts."""
     counts = _mostly_the_last(experts, rows - 5)
     _check_experts(_block(), rows, counts, i, o, True, 0.1, "plain", dtype)
+
+
+# ---------------------------------------------------------------------------
+# beside autograd
+# ---------------------------------------------------------------------------
+
+def test_writing_in_place_counts_as_a_modification():
+    """A tensor that autograd saved and dropout then wrote over must not be used
+    in the backward pass; one that requires gradients is not written over."""
+    block = _block()
+    w = torch.ones(8, 8, device="cuda", requires_grad=True)
+    x = torch.ones(8, 8, device="cuda")
+    y = (w * x).sum()
+    block.dropout(x, 0.5, SEED, 0, out=x)
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        y.backward()
+    out = torch.empty(8, 8, device="cuda")
+    before = out._version
+    block.dropout(w, 0.5, SEED, 0, out=out)
+    assert out._version == before + 1 and not out.requires_grad
+    with pytest.raises(ValueError, match="out requires gradients"):
+        block.dropout(x, 0.5, SEED, 0, out=w)
+    assert (w == 1).all()
+    with torch.no_grad():
+        block.dropout(x, 0.5, SEED, 0, out=w)
+    assert torch.equal(w.detach(), block.dropout(x, 0.5, SEED, 0))
