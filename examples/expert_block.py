@@ -32,12 +32,14 @@ from paper_1710_02368_amd import block  # noqa: E402
 
 
 class ExpertBlocks:
-    """Parameters, one training step and the forward pass of the model."""
+    """Parameters, one training step and the forward pass of the model.  The
+    pass and its gradients can be captured into a graph after a first eager call
+    with as many rows; replays draw the masks of steps_done at the time."""
 
     def __init__(self, inputs, classes, blocks=2, width=256, hidden=256, experts=8, k=2, rate=0.1, alpha=0.5,
                  dtype=torch.bfloat16, seed=1):
         self.blocks, self.k, self.rate, self.alpha, self.dtype, self.seed = blocks, k, rate, alpha, dtype, seed
-        self.steps_done = torch.zeros(1, dtype=torch.int32, device="cuda")  # moves the masks on, also in a graph
+        self.steps_done = torch.zeros(1, dtype=torch.int32, device="cuda")  # moves the masks on
         g = torch.Generator().manual_seed(seed)
         normal = lambda *shape: (torch.randn(*shape, generator=g) * (2.0 / shape[-1]) ** 0.5).cuda()
         p = {"in.w": normal(1, width, inputs), "in.b": torch.zeros(1, width, device="cuda"),
@@ -51,10 +53,14 @@ class ExpertBlocks:
                       f"{b}.pre": torch.ones(width, device="cuda")})
         self.params = p
         self.copies = {n: t.to(dtype) for n, t in p.items() if t.dim() == 3}  # what the products read
+        self._offsets = {}
 
     def _all_rows(self, rows):
-        """The offsets of a product with one expert."""
-        return torch.tensor([0, rows], dtype=torch.int32, device="cuda")
+        """The offsets of a product with one expert, made once for a number of
+        rows (by a copy from the host, which a graph cannot hold)."""
+        if rows not in self._offsets:
+            self._offsets[rows] = torch.tensor([0, rows], dtype=torch.int32, device="cuda")
+        return self._offsets[rows]
 
     def forward(self, x, train=False):
         """Logits, and with train what the backward pass needs."""
