@@ -2,22 +2,19 @@
 #pragma once
 
 #include "block_common.h"
+#include "experts_rules.h"
 #include "row_tiles.h"
 
 namespace agn {
-
-enum { PROD_FWD = 0, PROD_DX = 1, PROD_DW = 2 };
 
 // One of the three products over all experts (all sizes below 2^31):
 //   FWD: out[r][n] = epilogue(sum_k a[r][k] b_e[n][k])    a = x,  b = w
 //   DX:  out[r][n] = epilogue(sum_k a[r][k] b_e[k][n])    a = dy, b = w
 //   DW:  out_e[m][n] = sum_r a[r][m] b[r][n]              a = dy, b = x
-struct ProductArgs {
+struct ProductArgs : ProductSizes {
   const void *a, *b;
   int64_t lda, ldb, bstride;  // bstride: from one expert's b to the next (FWD, DX)
   bool a_pad, b_pad;          // rows go on with zeros to a multiple of eight
-  int rows, experts;
-  int M, N, K;                // M: DW only; K: not DW
   const int32_t* offsets;
   void* out;
   int64_t ldo;
@@ -33,14 +30,16 @@ struct ProductArgs {
   float *parts, *parts_bias;
 };
 
-hipError_t launch_product_bf16(int prod, const ProductArgs& g, hipStream_t s);
-// weight-gradient tiles an expert, and how many workgroups fill the chip
-int weight_tiles_bf16(const ProductArgs& g, int* fill);
-int weight_tiles_f32(const ProductArgs& g, int* fill);
+// operands whose every chunk of eight is a 16-byte aligned piece of one row
+inline bool direct_ok(int prod, const ProductArgs& g) {
+  if ((((uintptr_t)g.a | (uintptr_t)g.b) & 15) || g.lda % 8 || g.ldb % 8 || g.bstride % 8) return false;
+  return whole_chunks(prod, g, g.a_pad, g.b_pad);
+}
 
-bool product_few_ok(int prod, int dtype, const ProductArgs& g);
-hipError_t launch_product_few(int dtype, const ProductArgs& g, hipStream_t s);
-hipError_t launch_product_f32(int prod, const ProductArgs& g, hipStream_t s);
+// (k: as product_kernel chose for this product)
+hipError_t launch_product_bf16(int prod, const ProductKernel& k, const ProductArgs& g, hipStream_t s);
+hipError_t launch_product_f32(int prod, const ProductKernel& k, const ProductArgs& g, hipStream_t s);
+hipError_t launch_product_few(const ProductKernel& k, int dtype, const ProductArgs& g, hipStream_t s);
 
 constexpr int kTailBlocks = 64;  // workgroups that clear the output rows of no expert
 
@@ -136,10 +135,6 @@ __device__ __forceinline__ Raw8<T> load_gate(const ProductArgs& g, int r, int c)
 
 inline int64_t weight_parts_most(const ProductArgs& g) {
   return g.part_rows ? g.rows / g.part_rows + g.experts : g.experts;
-}
-
-inline int row_tiles_most(const ProductArgs& g, int TR) {
-  return g.rows / TR + (g.experts < g.rows ? g.experts : g.rows);
 }
 
 }  // namespace

@@ -84,50 +84,9 @@ void pad_rows(const agn_rows& m, int64_t rows, int cols, const agn_rows& out, hi
                      (const uint16_t*)m.p, m.ld, rows, cols, (uint16_t*)out.p, out.ld);
 }
 
-// Copies of bfloat16 operands whose width is no multiple of eight, so that the
-// direct loads take them.  Without, 16-byte loads at any alignment go through
-// registers into 128 x 128 tiles at 510 to 620 TFLOP/s, with them the products
-// run at 800 to 1000.  They pay where the sums are long for what is copied (at
-// about 4.5 TB/s); us without : with, copies included:
-//   16108 rows of 8 experts, 2047 -> 2049: forward 270 : 228, input gradient 269 :
-//     216, weight gradient 248 : 227 (either with its own copies); 12000 of 2,
-//     4001 -> 1001: 174 : 150, 204 : 162, 175 : 181;
-//   16108 of 8, 1001 -> 1003 forward 82 : 82 at the bound (not copied), 515 -> 1003
-//     its gradients 55 : 55 and 70 : 73.
-// Up to 1 GiB; an operand beyond is read as it is.
-struct Copies {
-  int64_t x, w, dy;  // bytes of each, 0: none
-  int64_t total() const { return x + w + dy; }
-};
-Copies copies(bool grad, int64_t rows, int64_t experts, int64_t inputs, int64_t outputs, int dtype) {
-  Copies c{};
-  if (dtype != AGN_BF16 || rows / experts < 512 || inputs < 256 || outputs < 256) return c;
-  const bool xw = inputs % 8, y = grad && outputs % 8;
-  const int64_t ip = (inputs + 7) / 8 * 8, op = (outputs + 7) / 8 * 8;
-  const double moved = (xw ? (double)(rows + experts * outputs) * inputs : 0) + (y ? (double)rows * outputs : 0);
-  if (moved == 0 || (double)rows * inputs * outputs < (grad ? 400 : 800) * moved) return c;
-  if (xw) {
-    c.x = rows * ip * 2;
-    c.w = experts * outputs * ip * 2;
-  }
-  if (y) c.dy = rows * op * 2;
-  if (c.total() > (INT64_C(1) << 30)) return Copies{};
-  return c;
-}
 // what a product reads: the operand, or its copy at `at` of so many bytes
 agn_rows operand(const agn_rows& m, int64_t bytes, int cols, char* at) {
   return bytes ? agn_rows{at, (cols + 7) / 8 * 8} : m;
-}
-
-// Rows a part of the weight gradients' sums: none where the tiles fill the
-// chip (then a part's float32 tile, written and read again, costs more than
-// the better balance gives), else parts of at least 512 rows that fill it twice.
-int weight_part_rows(const ProductArgs& g, int dtype) {
-  int fill;
-  const int64_t per = dtype == AGN_BF16 ? weight_tiles_bf16(g, &fill) : weight_tiles_f32(g, &fill);
-  if (per * g.experts >= fill) return 0;
-  const int64_t rows = std::max<int64_t>(512, (g.rows * per / (2 * fill) + 63) / 64 * 64);
-  return g.rows > rows ? (int)rows : 0;
 }
 
 const char* sizes_error(int64_t rows, int32_t experts, int32_t inputs, int32_t outputs, int32_t dtype) {
@@ -147,9 +106,12 @@ const char* weights_error(const agn_rows& w, int32_t experts, int32_t inputs, in
   return rows_error(w, (int64_t)experts * outputs, inputs, dtype);
 }
 
-hipError_t product(int prod, int dtype, const ProductArgs& g, hipStream_t s) {
-  if (product_few_ok(prod, dtype, g)) return launch_product_few(dtype, g, s);
-  return dtype == AGN_BF16 ? launch_product_bf16(prod, g, s) : launch_product_f32(prod, g, s);
+hipError_t product(int prod, const ProductKernel& k, int dtype, const ProductArgs& g, hipStream_t s) {
+  if (k.few) return launch_product_few(k, dtype, g, s);
+  return dtype == AGN_BF16 ? launch_product_bf16(prod, k, g, s) : launch_product_f32(prod, k, g, s);
+}
+ProductKernel kernel_of(int prod, int dtype, const ProductArgs& g) {
+  return product_kernel(prod, dtype, g, direct_ok(prod, g));
 }
 
 }  // namespace
@@ -180,10 +142,8 @@ extern "C" int64_t agn_experts_backward_workspace(int64_t rows, int32_t experts,
     g.experts = experts;
     g.M = outputs;
     g.N = inputs;
-    g.lda = g.ldb = aligned ? 8 : 1;
-    g.a_pad = c.dy > 0;
-    g.b_pad = c.x > 0;
-    g.part_rows = weight_part_rows(g, dtype);
+    const bool direct = aligned && whole_chunks(PROD_DW, g, c.dy > 0, c.x > 0);
+    g.part_rows = weight_part_rows(g, product_kernel(PROD_DW, dtype, g, direct));
     if (g.part_rows) need = std::max(need, weight_parts_most(g) * ((int64_t)outputs * inputs + outputs) * (int64_t)sizeof(float));
   }
   return c.total() + need;
@@ -229,7 +189,7 @@ extern "C" int agn_experts(const agn_experts_args* a, void* stream) {
   g.bias = a->bias;
   g.relu = a->relu;
   g.mask = mask_args(a->mask);
-  const hipError_t e = product(PROD_FWD, a->dtype, g, (hipStream_t)stream);
+  const hipError_t e = product(PROD_FWD, kernel_of(PROD_FWD, a->dtype, g), a->dtype, g, (hipStream_t)stream);
   return e == hipSuccess ? AGN_OK : block_fail(AGN_EHIP, fn, hipGetErrorString(e));
 }
 
@@ -288,8 +248,9 @@ extern "C" int agn_experts_backward(const agn_experts_grad_args* a, void* stream
   dw.ldo = a->inputs;
   dw.dbias = a->dbias;
   int64_t need = want_dx || a->dw ? cp.total() : 0;
+  const ProductKernel dw_kernel = kernel_of(PROD_DW, a->dtype, dw);
   if (a->dw) {
-    dw.part_rows = weight_part_rows(dw, a->dtype);
+    dw.part_rows = weight_part_rows(dw, dw_kernel);
     if (dw.part_rows) {
       const int64_t parts = weight_parts_most(dw);
       need += parts * ((int64_t)dw.M * dw.N + dw.M) * (int64_t)sizeof(float);
@@ -304,8 +265,8 @@ extern "C" int agn_experts_backward(const agn_experts_grad_args* a, void* stream
   if (cp.x && a->dw) pad_rows(a->x, a->rows, a->inputs, x, s);
   if (cp.w && want_dx) pad_rows(a->w, (int64_t)a->experts * a->outputs, a->inputs, w, s);
   hipError_t e = hipSuccess;
-  if (want_dx) e = product(PROD_DX, a->dtype, dx, s);
-  if (e == hipSuccess && a->dw) e = product(PROD_DW, a->dtype, dw, s);
+  if (want_dx) e = product(PROD_DX, kernel_of(PROD_DX, a->dtype, dx), a->dtype, dx, s);
+  if (e == hipSuccess && a->dw) e = product(PROD_DW, dw_kernel, a->dtype, dw, s);
   if (e == hipSuccess && a->dw && dw.part_rows) {
     const int per = (int)(((int64_t)dw.M * dw.N + 1023) / 1024);
     hipLaunchKernelGGL(sum_weight_parts_kernel, dim3(dw.experts * per), dim3(256), 0, s, dw, per);

@@ -44,7 +44,6 @@ typedef short i16x4 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) i16x4 lds_i16x4;
 
 constexpr int BK = 64, NT = 512;
-constexpr int kCUs = 256;
 
 template <int TR>
 struct Geo {
@@ -67,7 +66,7 @@ __device__ __forceinline__ int ks_byte(int k, int c) { return ((TR / 8) * k + (c
 // a chunk at the end of a row being loaded as the row's last eight elements
 // and moved down when it is written to LDS; or element by element (TINY),
 // where rows have fewer than eight.
-enum { DIRECT, STAGED, TINY };
+enum { DIRECT = WAY_DIRECT, STAGED = WAY_STAGED, TINY = WAY_TINY };
 
 // One operand's loads (instruction j = IPW wave + u; lane l fills LDS chunk
 // 64 j + l).  Outer indices past the edge repeat the last row or chunk (they
@@ -369,14 +368,10 @@ int row_blocks(const ProductArgs& g) {
   return row_tiles_most(g, 256) * ((g.N + 255) / 256) + 3 * kCUs / 2;
 }
 
-template <int TR>
-__host__ __device__ inline int weight_tiles(const ProductArgs& g) {
-  return ((g.M + TR - 1) / TR) * ((g.N + TR - 1) / TR);
-}
 template <int TR, int WAY>
 __device__ __forceinline__ void weight_tile(const ProductArgs& g, int pid, char* lds) {
   const int tn = (g.N + TR - 1) / TR;
-  const WeightTile w = weight_tile_of(g, pid, weight_tiles<TR>(g));
+  const WeightTile w = weight_tile_of(g, pid, weight_tiles(g, TR, TR));
   if (w.e < 0) return;
   const int m0 = (w.t / tn) * TR, n0 = (w.t % tn) * TR;
   tile<PROD_DW, TR, WAY>(g, w.e, m0, g.M, n0, w.rows, (const uint16_t*)g.a + w.r0 * g.lda + m0,
@@ -409,65 +404,28 @@ __global__ __launch_bounds__(NT, 4) void product_mid_kernel(ProductArgs g) {
   if (t.e >= 0) row_tile<PROD, TR, WAY>(g, t.e, t.r0, t.rend, (logical % tn) * TR, lds);
 }
 
-// Operands whose every chunk of eight is a 16-byte aligned piece of one row.
-bool direct_ok(int prod, const ProductArgs& g) {
-  if ((((uintptr_t)g.a | (uintptr_t)g.b) & 15) || g.lda % 8 || g.ldb % 8 || g.bstride % 8) return false;
-  const bool a = g.a_pad || (prod == PROD_DW ? g.M : g.K) % 8 == 0, b = g.b_pad || (prod == PROD_FWD ? g.K : g.N) % 8 == 0;
-  return a && b;
-}
-
-// every operand's rows have eight elements
-bool rows_of_eight(int prod, const ProductArgs& g) {
-  return (prod == PROD_DW ? g.M : g.K) >= 8 && (prod == PROD_FWD || g.N >= 8);
-}
-
-// 256 x 256 tiles, or 128 x 128 where the matrix is narrow, rows are few for
-// the number of experts (much of the larger tiles would be empty, or their
-// stores outlast their sums) or tiles are few for the 256 CUs.  us, 256 against
-// 128 (row products: tiles counted as row_tiles_most does):
-//   forward: 16108 rows of 8 experts, 2048 -> 2048 (568 tiles) 157 : 190; 8192 of
-//     8, 1536 -> 1536 (240) 48 : 56; 1024 -> 1024 (160) 34 : 34, its input gradient
-//     32 : 35; 16000 of 8, 512 -> 512 (140) 24 : 17; 4096 of 8, 1024 -> 1024 (96)
-//     30 : 21; 16108 of 64, 1024 -> 1024 75 : 61;
-//   weight gradients: 16108 of 8, 2048 -> 2048 (512 tiles) 136 : 167; 8000 of 4,
-//     2048 -> 2048 (256) 88 : 96; 4000 of 12, 1024 -> 1024 (192) 36 : 28; 4000 of 8,
-//     1024 -> 512 (64) 33 : 25; 500 of 8, 256 -> 256 (8) 13 : 6; 16108 of 64, 1024 ->
-//     1024 (252 rows an expert) 103 : 122; 4000 of 18 (222) 38 : 34; 4000 of 36
-//     (111) 56 : 46.
-bool big_tiles(int prod, const ProductArgs& g) {
-  if (g.N < 256) return false;
-  if (prod == PROD_DW)
-    return g.M >= 256 && g.rows / g.experts >= 240 && g.experts * (int64_t)weight_tiles<256>(g) >= kCUs;
-  return g.rows / g.experts >= 512 && row_tiles_most(g, 256) * (int64_t)((g.N + 255) / 256) >= 144;
-}
-
 template <int PROD, int WAY>
 void launch_mid(const ProductArgs& g, hipStream_t s) {
-  const int blocks = PROD == PROD_DW ? (int)weight_parts_most(g) * weight_tiles<128>(g)
+  const int blocks = PROD == PROD_DW ? (int)weight_parts_most(g) * weight_tiles(g, 128, 128)
                                      : row_tiles_most(g, 128) * ((g.N + 127) / 128) + kTailBlocks;
   hipLaunchKernelGGL((product_mid_kernel<PROD, WAY>), dim3(blocks), dim3(NT), 0, s, g);
 }
 
 template <int PROD>
-void launch(const ProductArgs& g, hipStream_t s) {
-  if (!direct_ok(PROD, g)) return rows_of_eight(PROD, g) ? launch_mid<PROD, STAGED>(g, s) : launch_mid<PROD, TINY>(g, s);
-  if (!big_tiles(PROD, g)) return launch_mid<PROD, DIRECT>(g, s);
-  const int blocks = PROD == PROD_DW ? (int)weight_parts_most(g) * weight_tiles<256>(g) : row_blocks(g) + kTailBlocks;
+void launch(const ProductKernel& k, const ProductArgs& g, hipStream_t s) {
+  if (k.way == WAY_STAGED) return launch_mid<PROD, STAGED>(g, s);
+  if (k.way == WAY_TINY) return launch_mid<PROD, TINY>(g, s);
+  if (k.tm == 128) return launch_mid<PROD, DIRECT>(g, s);
+  const int blocks = PROD == PROD_DW ? (int)weight_parts_most(g) * weight_tiles(g, 256, 256) : row_blocks(g) + kTailBlocks;
   hipLaunchKernelGGL(product_big_kernel<PROD>, dim3(blocks), dim3(NT), 0, s, g);
 }
 
 }  // namespace
 
-int weight_tiles_bf16(const ProductArgs& g, int* fill) {
-  const bool big = direct_ok(PROD_DW, g) && big_tiles(PROD_DW, g);
-  *fill = big ? kCUs : 2 * kCUs;
-  return big ? weight_tiles<256>(g) : weight_tiles<128>(g);
-}
-
-hipError_t launch_product_bf16(int prod, const ProductArgs& g, hipStream_t s) {
-  if (prod == PROD_DW) launch<PROD_DW>(g, s);
-  else if (prod == PROD_FWD) launch<PROD_FWD>(g, s);
-  else launch<PROD_DX>(g, s);
+hipError_t launch_product_bf16(int prod, const ProductKernel& k, const ProductArgs& g, hipStream_t s) {
+  if (prod == PROD_DW) launch<PROD_DW>(k, g, s);
+  else if (prod == PROD_FWD) launch<PROD_FWD>(k, g, s);
+  else launch<PROD_DX>(k, g, s);
   return hipGetLastError();
 }
 

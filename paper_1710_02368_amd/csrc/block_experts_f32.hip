@@ -111,11 +111,6 @@ struct Staged {
   }
 };
 
-template <int TM, int TN>
-__host__ __device__ inline int weight_tiles(const ProductArgs& g) {
-  return ((g.M + TM - 1) / TM) * ((g.N + TN - 1) / TN);
-}
-
 template <int PROD, int TM, int TN, bool TINY>
 __global__ __launch_bounds__(NT) void product_kernel(ProductArgs g) {
   using G = Geo<TM, TN>;
@@ -129,7 +124,7 @@ __global__ __launch_bounds__(NT) void product_kernel(ProductArgs g) {
   const float *pa, *pb;
   float *dw = nullptr, *dbias = nullptr;
   if (PROD == PROD_DW) {
-    const WeightTile w = weight_tile_of(g, blockIdx.x, weight_tiles<TM, TN>(g));
+    const WeightTile w = weight_tile_of(g, blockIdx.x, weight_tiles(g, TM, TN));
     if (w.e < 0) return;
     e = w.e;
     m0 = (w.t / tn) * TM;
@@ -277,66 +272,27 @@ __global__ __launch_bounds__(NT) void product_kernel(ProductArgs g) {
   }
 }
 
-// 128 x 128 tiles where there are many (a CU holds two: with few of them the
-// last round is mostly empty)
-constexpr int kMany = 2048;
-bool large_tiles(int prod, const ProductArgs& g) {
-  const int64_t tn = (g.N + 127) / 128;
-  return (prod == PROD_DW ? (int64_t)g.experts * weight_tiles<128, 128>(g) : row_tiles_most(g, 128) * tn) >= kMany;
-}
-
-// 64 x 32 rather than 64 x 64.  A half tile's step takes a little more than
-// half a tile's, but with few tiles the chip's rounds come out better and less
-// of the edges is padding.  us, 64 x 64 against 64 x 32:
-//   forward, input gradient: 3330 rows of 5 experts, 517 -> 259, 28.0 : 19.5;
-//     2000 of 8, 1024 -> 1024, 67 : 61; 16000 of 8, 300 -> 300 (1330 tiles) 48 :
-//     46; 12000 of 8, 512 -> 512 (1560 tiles) 73 : 76;
-//   weight gradients, by the rounds of 256 tiles each takes: 8192 rows of 8,
-//     515 -> 515 (3 : 5 half) 80 : 69; 2048 of 2, 2048 -> 300 (2 : 3) 57 : 44; 12000
-//     of 8, 512 -> 512 (2 : 4) 76 : 81; 1500 of 30, 700 -> 700 (15 : 29) 51 : 59;
-//     where the 64 x 64 tiles do not make one round and would go in parts:
-//     3330 of 5, 517 -> 259 (425 half tiles) 34 : 24; 6000 of 4, 256 -> 500 (256)
-//     34 : 36.
-bool narrow_tiles(int prod, const ProductArgs& g) {
-  const int64_t t64 = prod == PROD_DW ? (int64_t)g.experts * weight_tiles<64, 64>(g)
-                                      : row_tiles_most(g, 64) * (int64_t)((g.N + 63) / 64);
-  if (prod != PROD_DW) return t64 < 1400;
-  const int64_t t32 = (int64_t)g.experts * weight_tiles<64, 32>(g);
-  return t64 < 256 ? t32 >= 320 : 11 * ((t32 + 255) / 256) < 20 * ((t64 + 255) / 256);
-}
-
 template <int PROD, int TM, int TN>
-void launch_tiles(const ProductArgs& g, hipStream_t s) {
-  const bool tiny = (PROD == PROD_DW ? g.M : g.K) < 4 || (PROD != PROD_FWD && g.N < 4);
+void launch_tiles(const ProductKernel& k, const ProductArgs& g, hipStream_t s) {
   const int tn = (g.N + TN - 1) / TN;
   const int blocks =
-      PROD == PROD_DW ? (int)weight_parts_most(g) * weight_tiles<TM, TN>(g) : row_tiles_most(g, TM) * tn + kTailBlocks;
-  hipLaunchKernelGGL((tiny ? product_kernel<PROD, TM, TN, true> : product_kernel<PROD, TM, TN, false>), dim3(blocks),
-                     dim3(NT), 0, s, g);
+      PROD == PROD_DW ? (int)weight_parts_most(g) * weight_tiles(g, TM, TN) : row_tiles_most(g, TM) * tn + kTailBlocks;
+  hipLaunchKernelGGL((k.way == WAY_TINY ? product_kernel<PROD, TM, TN, true> : product_kernel<PROD, TM, TN, false>),
+                     dim3(blocks), dim3(NT), 0, s, g);
 }
 template <int PROD>
-void launch(const ProductArgs& g, hipStream_t s) {
-  if (large_tiles(PROD, g)) launch_tiles<PROD, 128, 128>(g, s);
-  else if (narrow_tiles(PROD, g)) launch_tiles<PROD, 64, 32>(g, s);
-  else launch_tiles<PROD, 64, 64>(g, s);
+void launch(const ProductKernel& k, const ProductArgs& g, hipStream_t s) {
+  if (k.tm == 128) launch_tiles<PROD, 128, 128>(k, g, s);
+  else if (k.tn == 32) launch_tiles<PROD, 64, 32>(k, g, s);
+  else launch_tiles<PROD, 64, 64>(k, g, s);
 }
 
 }  // namespace
 
-int weight_tiles_f32(const ProductArgs& g, int* fill) {
-  *fill = 512;
-  if (large_tiles(PROD_DW, g)) return weight_tiles<128, 128>(g);
-  if (narrow_tiles(PROD_DW, g)) {
-    *fill = 256;
-    return weight_tiles<64, 32>(g);
-  }
-  return weight_tiles<64, 64>(g);
-}
-
-hipError_t launch_product_f32(int prod, const ProductArgs& g, hipStream_t s) {
-  if (prod == PROD_DW) launch<PROD_DW>(g, s);
-  else if (prod == PROD_FWD) launch<PROD_FWD>(g, s);
-  else launch<PROD_DX>(g, s);
+hipError_t launch_product_f32(int prod, const ProductKernel& k, const ProductArgs& g, hipStream_t s) {
+  if (prod == PROD_DW) launch<PROD_DW>(k, g, s);
+  else if (prod == PROD_FWD) launch<PROD_FWD>(k, g, s);
+  else launch<PROD_DX>(k, g, s);
   return hipGetLastError();
 }
 

@@ -8,9 +8,6 @@
 // The order of k within a sum is free, so that lane group g = lane / 16 takes
 // k 16g .. 16g+15 of a piece (8g .. 8g+7 in float32): its loads are adjacent
 // and a row's four groups read one 128-byte line.
-#include <algorithm>
-#include <cmath>
-
 #include "block_experts.h"
 
 namespace agn {
@@ -132,39 +129,9 @@ void launch(const ProductArgs& g, hipStream_t s) {
 
 }  // namespace
 
-// Where this kernel is taken (forward, us, this against the tiles' kernel):
-//   bfloat16, up to 512 rows, where an estimate of its time is the shorter one:
-//     it reads an expert's weights once for every 32 rows, at about 4.3 TB/s;
-//     the 128 x 128 tiles read them once, and a tile's chain of K takes 0.8 us
-//     a step of 64 however few they are.  Rows in equal parts are assumed.
-//     5 rows to 5 of 18 experts, 3428 -> 1885: 16 : 46; 64 rows of 8, 2048 -> 2048
-//     18 : 30, 256 rows 23 : 31, 512 rows 41 : 32; 64 rows of 4, 4096 -> 4096 34 :
-//     55, 256 rows of one 67 : 56; 64 of 64, 1024 -> 1024 33 : 25; 512 of one, 1024
-//     -> 512 7 : 13;
-//   float32, up to 8 rows an expert (64 of 8, 2048 -> 2048: 33 : 50; 64 of 64, 1024
-//     -> 1024: 63 : 96), up to 16 of at most 256 (128 of 8, 2048 -> 2048: 46 : 49; 64
-//     of 4, 4096 -> 4096: 86 : 96), or where the 64 x 64 tiles are at most 96 (8
-//     experts, 1024 -> 512: 256 rows 13 : 17; one, 1024 rows, 136 tiles, 25 : 17).
-// 16 rows x 16 columns a workgroup up to 16 rows, or 8 an expert, else 32 x 32.
-bool product_few_ok(int prod, int dtype, const ProductArgs& g) {
-  // (a launch has fewer than 2^32 threads)
-  if (prod != PROD_FWD || row_tiles_most(g, 16) * (int64_t)((g.N + 15) / 16) > 1 << 22) return false;
-  if (dtype == AGN_BF16) {
-    if (g.rows > 512) return false;
-    // estimated us of this kernel and of the 128 x 128 tiles', two a CU
-    const double used = std::min(g.experts, g.rows), weights = 2.0 * g.N * g.K;
-    const double here = 4 + used * ((g.rows / g.experts + 31) / 32 + (g.rows < g.experts)) * weights / 4.3e6;
-    const double rounds = std::ceil(row_tiles_most(g, 128) * (double)((g.N + 127) / 128) / 512);
-    return here < 5 + std::max(rounds * g.K / 80, used * weights / 5.2e6);
-  }
-  return g.rows <= 8 * (int64_t)g.experts || (g.rows <= 16 * (int64_t)g.experts && g.rows <= 256) ||
-         row_tiles_most(g, 64) * (int64_t)((g.N + 63) / 64) <= 96;
-}
-
-hipError_t launch_product_few(int dtype, const ProductArgs& g, hipStream_t s) {
-  const bool few = g.rows <= 16 || g.rows <= 8 * (int64_t)g.experts;
-  if (dtype == AGN_BF16) few ? launch<uint16_t, 1, 1>(g, s) : launch<uint16_t, 2, 2>(g, s);
-  else few ? launch<float, 1, 1>(g, s) : launch<float, 2, 2>(g, s);
+hipError_t launch_product_few(const ProductKernel& k, int dtype, const ProductArgs& g, hipStream_t s) {
+  if (dtype == AGN_BF16) k.tm == 16 ? launch<uint16_t, 1, 1>(g, s) : launch<uint16_t, 2, 2>(g, s);
+  else k.tm == 16 ? launch<float, 1, 1>(g, s) : launch<float, 2, 2>(g, s);
   return hipGetLastError();
 }
 

@@ -5,6 +5,7 @@ import pytest
 import torch
 
 from tests import block_oracle as O
+from tests.block_kernels import CASES
 from tests.helpers import require_gpu
 from tests.test_gpu_block import BOTH, DTYPES, SEED, _check_experts, _check_norms, _norms_case
 
@@ -132,6 +133,33 @@ def test_many_experts(experts, rows, i, o, dtype):
     """Few rows and many, nearly all of them in the last group of 64 experts."""
     counts = _mostly_the_last(experts, rows - 5)
     _check_experts(_block(), rows, counts, i, o, True, 0.1, "plain", dtype)
+
+
+@pytest.mark.parametrize("case", CASES, ids=[f"{c[0]}_{c[1]}rows_{len(c[2])}e_{c[3]}x{c[4]}" for c in CASES])
+def test_every_kernel_of_the_experts(case):
+    dtype, rows, counts, i, o = case
+    rate = 0.1 if rows * o < 1 << 21 else 0.0
+    _check_experts(_block(), rows, counts, i, o, True, rate, "plain", dtype)
+
+
+@BOTH
+def test_experts_of_many_rows_do_not_mix_rows(dtype):
+    """As with few rows: NaN and infinities of one expert's rows stay in its
+    outputs, in the tiles' kernels, aligned, odd and shorter than a load."""
+    block = _block()
+    for i, o in ((72, 40), (75, 41), (256, 256), (5, 300), (3, 300)):
+        counts = [330, 235, 220]
+        x, w, dy = (torch.randn(*s, generator=torch.Generator().manual_seed(n)).to(DTYPES[dtype]).cuda()
+                    for n, s in enumerate(((800, i), (3, o, i), (800, o))))
+        x[330:565], x[785:], dy[330:565], dy[785:] = float("nan"), float("inf"), float("inf"), float("nan")
+        off = torch.tensor([0, *np.cumsum(counts)], dtype=torch.int32, device="cuda")
+        h = block.experts(x, off, w)
+        dx, dw, db = block.experts_backward(x, dy, off, w)
+        for v in (h, dx):
+            assert torch.isfinite(v[:330]).all() and torch.isfinite(v[565:785]).all() and (v[785:] == 0).all()
+            assert not torch.isfinite(v[330:565]).any()
+        for v in (dw, db):
+            assert torch.isfinite(v[[0, 2]]).all() and not torch.isfinite(v[1]).any()
 
 
 # ---------------------------------------------------------------------------
