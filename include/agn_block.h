@@ -25,7 +25,9 @@
  *     at where a matrix has at most one row.  Sums, statistics and products
  *     are accumulated in float32; a bfloat16 output is rounded once, to
  *     nearest even.  Outputs must not overlap inputs unless a call says so.
- *   - Results do not depend on timing: the same inputs give the same bits.
+ *   - Results do not depend on timing: the same inputs give the same bits
+ *     (of the experts' products: with operands of the same alignment, which
+ *     has a part in the choice of kernel).
  */
 #ifndef AGN_BLOCK_H
 #define AGN_BLOCK_H
@@ -90,7 +92,9 @@ int agn_dropout(const agn_dropout_args* a, void* stream);
  *   u = norm(f) * w_post                 (u = f where w_post is NULL)
  *   residual' = residual + alpha * gate * mask * u
  *   h = norm(residual') * w_pre          (no h where w_pre is NULL)
- * row by row, with norm(v) = v / sqrt(mean(v^2) + eps).  f.p NULL: there is
+ * row by row, with norm(v) = v / sqrt(mean(v^2) + eps), the squares summed in
+ * float32 (a row whose sum passes its range has norm 0).  A dropped element
+ * adds 0 whatever its gate and weight are, also in the gradients.  f.p NULL: there is
  * no block before (residual' = residual, and residual_out is not written);
  * then w_pre must be given.  h is computed from the float32 residual'. */
 typedef struct {
@@ -284,7 +288,8 @@ int agn_experts(const agn_experts_args* a, void* stream);
  *     input_rate): the gradient of the sums before that ReLU.
  *   dw (experts x outputs x inputs floats, contiguous) = dy^T x over the
  *     expert's rows, zero for an expert without rows; dbias (experts x
- *     outputs floats) = the sums of dy over the expert's rows.
+ *     outputs floats) = the sums of dy over the expert's rows (in an order that
+ *     depends on whether dw is wanted too).
  * Each of dx.p, dw, dbias may be NULL: not wanted. */
 typedef struct {
   int64_t rows;

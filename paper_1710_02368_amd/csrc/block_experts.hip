@@ -212,8 +212,9 @@ extern "C" int agn_experts_backward(const agn_experts_grad_args* a, void* stream
   }
   const hipStream_t s = (hipStream_t)stream;
   const bool want_dx = a->dx.p && a->rows > 0;
-  // which operands are copied goes by the sizes alone, so that a gradient's
-  // bits do not depend on which others are wanted
+  // which operands are copied goes by the sizes alone, so that the bits of dx
+  // and dw do not depend on which others are wanted (dbias has an order of
+  // summation of its own where dw is not)
   const Copies cp = copies(true, a->rows, a->experts, a->inputs, a->outputs, a->dtype);
   char* ws = (char*)a->workspace;  // the copies of dy, x and w, then the parts
   const agn_rows dy = operand(a->dy, cp.dy, a->outputs, ws), x = operand(a->x, cp.x, a->inputs, ws + cp.dy),

@@ -6,13 +6,15 @@
 // alignment) into two LDS stages: the next step's loads are in flight during a
 // step's MFMAs.  (Two, three or four steps ahead were no faster: 3330 rows of
 // 5 experts, 517 -> 259, forward in 64 x 64 tiles 28 us with one, 30 to 31 with
-// more: MFMAs and whole rounds of tiles bound it.)  The tiles lie in LDS as
-// they are loaded, [outer][k] or [k][outer].  The order of k in a sum is free:
-// of eight k the lanes 0 .. 31 take the first four and the lanes 32 .. 63 the
+// more.)  The tiles lie in LDS as they are loaded, [outer][k] or [k][outer].
+// The order of k in a sum is free: of eight k the lanes 0 .. 31 take the first four and the lanes 32 .. 63 the
 // last, so that a lane's fragments of four MFMAs are one 16-byte read of a
 // K-contiguous tile; they are read while the MFMAs of the eight k before run.
-// 3330 rows of 5 experts, 517 -> 259: forward 20 us (46 TFLOP/s; the chip's
-// 256 CUs take 513 tiles), 8192 of 8, 2048 -> 2048: 644 us (107 TFLOP/s).
+// 3330 rows of 5 experts, 517 -> 259: forward 19 us (48 TFLOP/s), 8192 of 8, 2048
+// -> 2048: 622 us (110 TFLOP/s).  What bounds short sums is the latency of a
+// step: three workgroups of 64 x 32 lie on a CU (53 KB of LDS each), so that all
+// 425 to 513 tiles of the former's products are there at once, and the matrix
+// pipe is busy 20 to 29% of their time.
 #include <type_traits>
 
 #include "block_experts.h"

@@ -83,7 +83,7 @@ inline bool rows_of_eight(int prod, const ProductSizes& g) {
 // the number of experts (much of the larger tiles would be empty, or their
 // stores outlast their sums) or tiles are few for the 256 CUs.  us, 256 against
 // 128 (row products: tiles counted as row_tiles_most does):
-//   forward: 16108 rows of 8 experts, 2048 -> 2048 (568 tiles) 157 : 190; 8192 of
+//   forward: 16108 rows of 8 experts, 2048 -> 2048 (560 tiles) 157 : 190; 8192 of
 //     8, 1536 -> 1536 (240) 48 : 56; 1024 -> 1024 (160) 34 : 34, its input gradient
 //     32 : 35; 16000 of 8, 512 -> 512 (140) 24 : 17; 4096 of 8, 1024 -> 1024 (96)
 //     30 : 21; 16108 of 64, 1024 -> 1024 75 : 61;
@@ -99,23 +99,25 @@ inline bool big_tiles(int prod, const ProductSizes& g) {
   return g.rows / g.experts >= 512 && row_tiles_most(g, 256) * (int64_t)((g.N + 255) / 256) >= 144;
 }
 
-// float32: 128 x 128 tiles where there are many (a CU holds two: with few of them the
-// last round is mostly empty)
+// float32: 128 x 128 tiles where there are many (a CU holds two: with few of
+// them the last round is mostly empty)
 inline bool large_tiles(int prod, const ProductSizes& g) {
   const int64_t tn = (g.N + 127) / 128;
   return (prod == PROD_DW ? (int64_t)g.experts * weight_tiles(g, 128, 128) : row_tiles_most(g, 128) * tn) >= 2048;
 }
 
-// float32: 64 x 32 rather than 64 x 64.  A half tile's step takes a little more than
-// half a tile's, but with few tiles the chip's rounds come out better and less
-// of the edges is padding.  us, 64 x 64 against 64 x 32:
+// float32: 64 x 32 rather than 64 x 64.  A half tile's step takes a little more
+// than half a tile's, but more of them lie on a CU (three for two), with few
+// tiles the CUs share them more evenly, and less of the edges is padding.  us,
+// 64 x 64 against 64 x 32:
 //   forward, input gradient: 3330 rows of 5 experts, 517 -> 259, 28.0 : 19.5;
-//     2000 of 8, 1024 -> 1024, 67 : 61; 16000 of 8, 300 -> 300 (1330 tiles) 48 :
+//     2000 of 8, 1024 -> 1024, 67 : 61; 16000 of 8, 300 -> 300 (1290 tiles) 48 :
 //     46; 12000 of 8, 512 -> 512 (1560 tiles) 73 : 76;
-//   weight gradients, by the rounds of 256 tiles each takes: 8192 rows of 8,
+//   weight gradients, by an estimate that fits them, 20 a 64 x 64 tile a CU and
+//     11 a half tile (in brackets tiles a CU, rounded up): 8192 rows of 8,
 //     515 -> 515 (3 : 5 half) 80 : 69; 2048 of 2, 2048 -> 300 (2 : 3) 57 : 44; 12000
 //     of 8, 512 -> 512 (2 : 4) 76 : 81; 1500 of 30, 700 -> 700 (15 : 29) 51 : 59;
-//     where the 64 x 64 tiles do not make one round and would go in parts:
+//     where the 64 x 64 tiles are less than one a CU and would go in parts:
 //     3330 of 5, 517 -> 259 (425 half tiles) 34 : 24; 6000 of 4, 256 -> 500 (256)
 //     34 : 36.
 inline bool narrow_tiles(int prod, const ProductSizes& g) {
