@@ -2,8 +2,8 @@
 #pragma once
 
 #include "block_common.h"
-#include "experts_rules.h"
-#include "row_tiles.h"
+#include "block_experts_rules.h"
+#include "block_row_tiles.h"
 
 namespace agn {
 

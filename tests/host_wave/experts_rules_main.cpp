@@ -1,9 +1,9 @@
 // Prints the kernels that the experts' products of contiguous operands take
-// (experts_rules.h).  Reads lines of "dtype rows experts inputs outputs";
+// (block_experts_rules.h).  Reads lines of "dtype rows experts inputs outputs";
 // writes "forward | input gradient | weight gradient" for each.
 #include <cstdio>
 
-#include "experts_rules.h"
+#include "block_experts_rules.h"
 
 using namespace agn;
 

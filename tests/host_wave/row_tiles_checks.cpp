@@ -1,4 +1,4 @@
-// The experts' tile search (row_tiles.h) on the host: its 64 lanes run as
+// The experts' tile search (block_row_tiles.h) on the host: its 64 lanes run as
 // fibers that wait for each other at every wave function, and every tile
 // number's answer is compared with a plain walk over the experts.
 #include <ucontext.h>
@@ -76,7 +76,7 @@ using std::min;
 #define __device__
 #define __forceinline__ inline
 #define __builtin_amdgcn_readlane readlane
-#include "row_tiles.h"
+#include "block_row_tiles.h"
 
 struct Args {
   const int32_t* offsets;
